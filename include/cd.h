@@ -470,9 +470,10 @@ cd_status cd_distill_backward(int64_t B, int64_t T, int64_t V, int K, const void
  *   tokens [B,T]        as above, not NULL; a row without a token is not looked at
  * Checks as above, and 1 <= D < 2^21, hidden and weight 16-byte aligned, at most 2^22 tiles of
  * 256 x 256 in a product (B T V, B T D and V D up to about 2.7e11).  weight must be finite (a
- * non-finite element may make any result NaN).  A copy is made in the workspace of hidden where D is no multiple of 64 or rows are not evenly spaced and 16-byte
- * aligned, of weight where D or ld_weight is no multiple of 8, of either where its rows are
- * more than 2^21 elements apart.
+ * non-finite element may make any result NaN); what lies between its rows is not used.  A copy
+ * is made in the workspace of hidden where D is no multiple of 64 or rows are not evenly spaced
+ * and 16-byte aligned, of weight where D or ld_weight is no multiple of 8, of either where its
+ * rows are more than 2^21 elements apart.
  */
 
 /* Device workspace bytes of the two calls below (the forward's if backward == 0); 0 for invalid

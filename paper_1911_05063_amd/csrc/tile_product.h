@@ -13,8 +13,9 @@
 //    elements and each lane gets a column), and pairs of chunks are permuted by the row
 //    bits that such a read spans.
 // Rows of m or n beyond an operand's end are read at its last row, and are the caller's to
-// ignore.  At k beyond its end an operand gives other elements of its own; the caller makes the
-// other operand 0 there.
+// ignore.  At k beyond its end an operand gives other elements of its own (with k adjacent the
+// last ones of the same row: what lies between its rows is not its own, and may be anything);
+// the caller makes the other operand 0 there.
 //
 // The products run as 16 x 16 x 32 with the operands exchanged, so that a lane holds, for
 // one m (lane & 15), four adjacent n ((lane >> 4) * 4 ..): a row's values meet in few
@@ -70,10 +71,11 @@ struct Operand {
 constexpr int kStepK = 64;       // k of two halves
 
 // Staging and reading of one operand: kSize rows of m (or n) per tile, kWaves waves.  kTurn: k
-// may start anywhere and goes round.  kOnce: the operand is read past the caches.
+// may start anywhere and goes round.  kOnce: the operand is read past the caches.  kWhole: with k
+// adjacent, rows are whole steps of k.
 // A lane's places relative to the tile and the step are 32-bit offsets that stay the same from
 // step to step; the step moves a uniform pointer.
-template <typename E, int kSize, bool kAcross, int kWaves, bool kTurn, bool kOnce>
+template <typename E, int kSize, bool kAcross, int kWaves, bool kTurn, bool kOnce, bool kWhole>
 struct Stage {
     static constexpr int kK = kAcross ? kStepK / 2 : kStepK; // k at a time
     static constexpr int kBuffers = kAcross ? 4 : 2;
@@ -84,7 +86,8 @@ struct Stage {
     static constexpr int kBytes = kChunks * 16;
 
     const char *at;             // of the tile at the next load's k
-    const char *final;          // the operand's last 16 bytes
+    const char *final;          // m or n adjacent: the operand's last 16 bytes
+    uint32_t tail;              // k adjacent: bytes of a row in the load that its end cuts
     int64_t stride;             // bytes between loads
     int64_t round;              // kTurn: bytes of all loads
     int32_t until;              // kTurn: loads until the last k; then the first comes
@@ -99,10 +102,10 @@ struct Stage {
     {
         whole = static_cast<int32_t>(((kAcross ? op.rows : op.cols) - k0) / kK);
         stride = kK * (kAcross ? op.ld * 2 : 2);
-        final = reinterpret_cast<const char *>(op.data + (op.rows - 1) * op.ld + op.cols - 8);
         const int in_load = lane / kRowChunks, chunk = lane % kRowChunks;
         const uint32_t ld = static_cast<uint32_t>(op.ld) * 2;
         if (kAcross) {
+            final = reinterpret_cast<const char *>(op.data + (op.rows - 1) * op.ld + op.cols - 8);
             at = reinterpret_cast<const char *>(op.data + k0 * op.ld);
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
@@ -111,6 +114,7 @@ struct Stage {
                 off[i] = r * ld + static_cast<uint32_t>(c < op.cols ? c : op.cols - 8) * 2;
             }
         } else {
+            tail = static_cast<uint32_t>(op.cols % kK) * 2;
             const int64_t from = first < op.rows ? first : op.rows - 1;
             at = reinterpret_cast<const char *>(op.data + from * op.ld + k0);
             // Row bits 0..2 are in_load's: a load fills 8 rows.
@@ -132,9 +136,15 @@ struct Stage {
                 (__attribute__((address_space(3))) void *)(lds + (i * kWaves + wave) * 1024), 16,
                 static_cast<int>(o), 0, 0, kOnce ? 2 : 0);     // (2: non-temporal)
         };
-        if (__builtin_expect(whole > 0, 1)) {
+        if ((!kAcross && kWhole) || __builtin_expect(whole > 0, 1)) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) put(at, i, off[i]);
+        } else if (!kAcross) {      // past a row's end its last 16 bytes
+            const uint32_t lane = threadIdx.x & 63;
+            const uint32_t place = (lane % kRowChunks ^ (lane / kRowChunks & 7)) * 16;
+            const uint32_t back = place < tail ? 0 : place - (tail - 16);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) put(at, i, off[i] - back);
         } else {    // past the operand's end its last 16 bytes
             const char *from = min(at, final);
             const uint32_t last = static_cast<uint32_t>(min(final - from, int64_t(1) << 31));
@@ -192,7 +202,8 @@ struct Stage {
     }
 };
 
-// kTileM x kTileN per workgroup of kWavesM x kWavesN waves.
+// kTileM x kTileN per workgroup of kWavesM x kWavesN waves.  A's columns are a multiple of kStepK
+// where its k is adjacent; so are B's with kTurn.
 template <typename E, int kTileM, int kTileN, int kWavesM, int kWavesN, bool kAcrossA, bool kAcrossB,
           bool kTurn = false, bool kOnceB = false>
 struct TileProduct {
@@ -200,8 +211,8 @@ struct TileProduct {
     static constexpr int kThreads = kWaves * 64;
     static constexpr int kWaveM = kTileM / kWavesM, kWaveN = kTileN / kWavesN;
     static constexpr int kM = kWaveM / 16, kN = kWaveN / 16;
-    typedef Stage<E, kTileM, kAcrossA, kWaves, kTurn, false> A;
-    typedef Stage<E, kTileN, kAcrossB, kWaves, kTurn, kOnceB> B;
+    typedef Stage<E, kTileM, kAcrossA, kWaves, kTurn, false, true> A;
+    typedef Stage<E, kTileN, kAcrossB, kWaves, kTurn, kOnceB, kTurn> B;
 
     // Loads of a wave with every step (of 32 k) and with every other one.
     static constexpr int kEach = (kAcrossA ? A::kLoads : 0) + (kAcrossB ? B::kLoads : 0);

@@ -268,3 +268,27 @@ def test_refusals():
     for temperature in (0.0, -1.0, float("nan"), float("inf")):
         with pytest.raises(cd.CDError):
             cd.head_logprobs(h, w, t, temperature=temperature)
+
+
+@pytest.mark.parametrize("around", [float("nan"), float("inf"), 1e30])
+@pytest.mark.parametrize("T,D,V,ld", [(5, 72, 700, 200), (40, 8, 333, 16), (300, 1000, 333, 1024),
+                                      (129, 40, 257, 48), (3200, 40, 3300, 48)])
+def test_what_lies_between_the_rows_of_the_weights_is_not_used(T, D, V, ld, around):
+    # Rows of a multiple of 8, not of 64, and further apart than they are long.
+    rng = np.random.default_rng(T + D)
+    h, w, tokens = make(rng, T, D, V, "bf16")
+    wide = torch.full((V, ld), around, device="cuda").bfloat16()
+    for off in (0, 8):
+        if off + D <= ld:
+            wide[:] = around
+            wide[:, off:off + D] = w
+            got = check(h, wide[:, off:off + D], tokens, "bf16", grads=T < 1000)
+            # The same bits as of weights without a gap.
+            hg, wg, tg = h.clone().requires_grad_(), w.clone().requires_grad_(), torch.from_numpy(tokens).cuda()
+            lp, ent = cd.head_logprobs(hg, wg, tg)
+            assert torch.equal(lp, got[0]) and torch.equal(ent, got[1])
+            one = torch.ones_like(lp)
+            want = torch.autograd.grad([lp, ent], [hg, wg], [one, one])
+            view = wide[:, off:off + D].detach().requires_grad_()
+            some = torch.autograd.grad(cd.head_logprobs(hg, view, tg), [hg, view], [one, one])
+            assert all(torch.equal(a, b) for a, b in zip(some, want))
