@@ -252,15 +252,19 @@ struct HeadRow {
     int32_t pad;
 };
 
-// The power of 2 that takes the largest possible |dx| to about 2^14 (float16).  One workgroup.
-__global__ __launch_bounds__(1024) void scale_kernel(int32_t T, float lnv, float inv_temperature,
-                                                     const float *g_logprob,
+// The power of 2 that takes the largest possible |dx| to about 2^14 (float16), over what
+// head_rows_kernel takes: a row without a token or a gradient may come with any g.  One workgroup.
+__global__ __launch_bounds__(1024) void scale_kernel(int32_t T, int32_t V, float lnv,
+                                                     float inv_temperature, const int32_t *tokens,
+                                                     const ScoreRow *saved, const float *g_logprob,
                                                      const float *g_entropy, float *scale)
 {
     __shared__ float part[16];
     float most = 0.0f;
     for (int32_t i = threadIdx.x; i < T; i += 1024) {
-        float g = g_logprob ? fabsf(g_logprob[i]) : 0.0f;
+        const int32_t t = tokens[i];
+        if (t < 0 || saved[i].m == -INFINITY) continue;
+        float g = g_logprob && t < V ? fabsf(g_logprob[i]) : 0.0f;
         if (g_entropy) g += fabsf(g_entropy[i]) * (lnv + 1.0f);
         most = fmaxf(most, g * inv_temperature);
     }
@@ -704,8 +708,9 @@ hipError_t backward(const Head &x, const int32_t *tokens, float temperature, con
     if (x.dtype == CD_F16) {
         scale = at<float>(ws, l.scale);
         scale_kernel<<<1, 1024, 0, stream>>>(static_cast<int32_t>(l.rows),
-                                             logf(static_cast<float>(x.V)), inv, g_logprob, g_entropy,
-                                             scale);
+                                             static_cast<int32_t>(x.V),
+                                             logf(static_cast<float>(x.V)), inv, tokens, saved,
+                                             g_logprob, g_entropy, scale);
     }
     HeadRow *head_rows = at<HeadRow>(ws, l.head_rows);
     head_rows_kernel<<<static_cast<unsigned>(up(rows, kRowThreads) / kRowThreads), kRowThreads, 0,

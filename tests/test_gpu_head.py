@@ -292,3 +292,26 @@ def test_what_lies_between_the_rows_of_the_weights_is_not_used(T, D, V, ld, arou
             view = wide[:, off:off + D].detach().requires_grad_()
             some = torch.autograd.grad(cd.head_logprobs(hg, view, tg), [hg, view], [one, one])
             assert all(torch.equal(a, b) for a, b in zip(some, want))
+
+
+@pytest.mark.parametrize("T", [40, 300])
+@pytest.mark.parametrize("big", [1e6, 1e30, float("inf"), float("nan")])
+def test_float16_gradients_of_rows_that_take_none_do_not_scale_the_others(T, big):
+    rng = np.random.default_rng(21)
+    h, w, tokens = make(rng, T, 64, 2000, "f16")
+    tokens[3], tokens[5] = -1, 2000             # no token; one past the vocabulary
+    tg = torch.from_numpy(tokens).cuda()
+    none, past = tg < 0, tg >= 2000
+
+    def grads(gl, ge):
+        a, b = h.clone().requires_grad_(), w.clone().requires_grad_()
+        return torch.autograd.grad(cd.head_logprobs(a, b, tg), [a, b], [gl, ge])
+
+    gl = torch.from_numpy(rng.normal(size=T).astype(np.float32)).cuda() * 2.0 ** -13
+    ge = gl.flip(0) * 0.1
+    clean = torch.where(none | past, 0.0, gl), torch.where(none, 0.0, ge)
+    want = grads(*clean)
+    assert want[0].any() and want[1].any()
+    got = grads(torch.where(none | past, big, gl), torch.where(none, big, ge))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
