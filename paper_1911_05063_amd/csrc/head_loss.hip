@@ -253,7 +253,8 @@ struct HeadRow {
 };
 
 // The power of 2 that takes the largest possible |dx| to about 2^14 (float16), over what
-// head_rows_kernel takes: a row without a token or a gradient may come with any g.  One workgroup.
+// head_rows_kernel takes: a row without a token or a gradient may come with any g.  Nor do rows count
+// whose g is not finite: their d/d hidden is not at any scale, the other rows' is.  One workgroup.
 __global__ __launch_bounds__(1024) void scale_kernel(int32_t T, int32_t V, float lnv,
                                                      float inv_temperature, const int32_t *tokens,
                                                      const ScoreRow *saved, const float *g_logprob,
@@ -266,7 +267,8 @@ __global__ __launch_bounds__(1024) void scale_kernel(int32_t T, int32_t V, float
         if (t < 0 || saved[i].m == -INFINITY) continue;
         float g = g_logprob && t < V ? fabsf(g_logprob[i]) : 0.0f;
         if (g_entropy) g += fabsf(g_entropy[i]) * (lnv + 1.0f);
-        most = fmaxf(most, g * inv_temperature);
+        g *= inv_temperature;
+        if (g < INFINITY) most = fmaxf(most, g);
     }
     most = group_max<64>(most);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
@@ -274,7 +276,7 @@ __global__ __launch_bounds__(1024) void scale_kernel(int32_t T, int32_t V, float
     if (threadIdx.x == 0) {
         for (int i = 1; i < 16; ++i) most = fmaxf(most, part[i]);
         int e = 0;
-        if (most > 0.0f && most < INFINITY) e = 14 - ilogbf(most);
+        if (most > 0.0f) e = 14 - ilogbf(most);
         e = e > 100 ? 100 : e < -100 ? -100 : e;
         scale[0] = ldexpf(1.0f, e);
         scale[1] = ldexpf(1.0f, -e);

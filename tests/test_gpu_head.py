@@ -315,3 +315,23 @@ def test_float16_gradients_of_rows_that_take_none_do_not_scale_the_others(T, big
     got = grads(torch.where(none | past, big, gl), torch.where(none, big, ge))
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("big", [float("inf"), float("nan")])
+def test_a_float16_gradient_that_is_not_finite_stays_in_its_row(big):
+    rng = np.random.default_rng(22)
+    h, w, tokens = make(rng, 40, 64, 2000, "f16")
+    tokens = np.abs(tokens)
+    tg = torch.from_numpy(tokens).cuda()
+
+    def grad(gl):
+        a = h.clone().requires_grad_()
+        return torch.autograd.grad(cd.head_logprobs(a, w, tg)[0], a, gl)[0]
+
+    gl = torch.from_numpy(rng.normal(size=40).astype(np.float32)).cuda() * 2.0 ** -13
+    gl[11] = 0.0
+    want = grad(gl)
+    gl[11] = big
+    got = grad(gl)
+    rest = torch.arange(40, device="cuda") != 11
+    assert torch.equal(got[rest], want[rest]) and not torch.isfinite(got[11]).any()
