@@ -34,6 +34,7 @@ import os
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 __all__ = [
     "CDError", "LIB_PATH", "library", "workspace_bytes", "workspace_bytes_best", "nn_distance",
@@ -693,9 +694,15 @@ def _float_tensor(t: torch.Tensor, name: str) -> int:
     return _DTYPES[t.dtype]
 
 
+def _tangent(t) -> bool:
+    return isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None
+
+
 def _differentiable(*tensors) -> bool:
-    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad
-                                           for t in tensors)
+    """Whether a call has to go through autograd: for a gradient, or, with a tensor that
+    carries a tangent, for its refusal of forward-mode derivatives."""
+    return any(isinstance(t, torch.Tensor) and t.requires_grad and torch.is_grad_enabled()
+               or _tangent(t) for t in tensors)
 
 
 def _logit_rows(x: torch.Tensor):
@@ -841,7 +848,7 @@ def distill_topk(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logi
     temperature over the row's entries (teacher_token [..., K] int32, negative: absent), p
     that of logits [..., V] / temperature.  Differentiable in the logits.  The top_token
     and top_logprob of token_logprobs(teacher_logits, top=K) serve as the teacher's entries."""
-    if _differentiable(logits):
+    if _differentiable(logits) or _tangent(teacher_logit):
         return DistillTopK.apply(logits, teacher_token, teacher_logit, float(temperature))
     return _distill_topk(logits, teacher_token, teacher_logit, float(temperature), False)[0]
 
