@@ -705,6 +705,26 @@ def _differentiable(*tensors) -> bool:
                or _tangent(t) for t in tensors)
 
 
+class _FirstOrder(torch.autograd.Function):
+    """A gradient, as it is, that refuses to be differentiated with respect to `of`."""
+
+    @staticmethod
+    def forward(ctx, grad, *of):
+        return grad
+
+    @staticmethod
+    def backward(ctx, _g):
+        raise RuntimeError("the token losses have no second derivatives")
+
+
+def _first_order(grad: Optional[torch.Tensor], *of) -> Optional[torch.Tensor]:
+    """What a backward returns: under create_graph it depends on `of`, unknown to autograd
+    (torch's once_differentiable looks at the upstream gradients alone)."""
+    if grad is None or not torch.is_grad_enabled():
+        return grad
+    return _FirstOrder.apply(grad, *of)
+
+
 def _logit_rows(x: torch.Tensor):
     """(x, B, T, V, stride_b, stride_t): the rows of x [..., V], read in place where
     the elements of a row are adjacent and two strides reach all rows."""
@@ -780,7 +800,7 @@ class TokenLogprobs(torch.autograd.Function):
                 B, T, V, _ptr(x), _DTYPES[logits.dtype], sb, st, _ptr(tokens), ctx.temperature,
                 _ptr(saved), _ptr(gl), _ptr(ge), _ptr(gx), _stream(dev)),
                 "cd_token_logprobs_backward")
-        return gx, None, None, None
+        return _first_order(gx, logits, g_logprob, g_entropy), None, None, None
 
 
 def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, top: int = 0,
@@ -839,7 +859,7 @@ class DistillTopK(torch.autograd.Function):
                 B, T, V, ids.shape[-1], _ptr(x), _DTYPES[logits.dtype], sb, st, _ptr(ids), _ptr(tl),
                 _DTYPES[tl.dtype], ctx.temperature, _ptr(saved), _ptr(g), _ptr(gx), _stream(dev)),
                 "cd_distill_backward")
-        return gx, None, None, None
+        return _first_order(gx, logits, g_loss), None, None, None
 
 
 def distill_topk(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_logit: torch.Tensor,
@@ -934,7 +954,8 @@ class HeadLogprobs(torch.autograd.Function):
                                                  ctx.temperature, _ptr(saved), _ptr(gl), _ptr(ge),
                                                  _ptr(gh), _ptr(gw), _ptr(ws), need, _stream(dev)),
                    "cd_head_logprobs_backward")
-        return gh, gw, None, None
+        of = hidden, weight, g_logprob, g_entropy
+        return _first_order(gh, *of), _first_order(gw, *of), None, None
 
 
 def head_logprobs(hidden: torch.Tensor, weight: torch.Tensor, tokens: torch.Tensor,
