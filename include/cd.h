@@ -382,7 +382,7 @@ cd_status cd_emd_backward(int64_t B, int64_t N, int64_t M, const float *X, const
  *    make the row's results NaN.
  *  - Checks (else CD_ERR_INVALID_ARG, nothing launched): B, T >= 0, B * T < 2^31,
  *    1 <= V < 2^31, strides >= 0, a known dtype, temperature positive and finite
- *    (and 1 / temperature finite).  B * T == 0 is a no-op.
+ *    (and log2(e) / temperature finite).  B * T == 0 is a no-op.
  *  - Results are bitwise reproducible from run to run.
  */
 typedef enum { CD_F32 = 0, CD_BF16 = 1, CD_F16 = 2 } cd_dtype;

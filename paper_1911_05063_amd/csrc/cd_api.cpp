@@ -471,8 +471,9 @@ static cd_status check_rows(int64_t B, int64_t T, int64_t V, cd_dtype dtype)
 
 static cd_status check_temperature(float t)
 {
-    if (!positive_finite(t) || !std::isfinite(1.0f / t))
-        return invalid("temperature must be positive and finite, and so its inverse");
+    // (log2(e) / t is what the kernels multiply by)
+    if (!positive_finite(t) || !std::isfinite(1.4426950408889634f / t))
+        return invalid("temperature must be positive and finite, and so log2(e) / temperature");
     return CD_OK;
 }
 

@@ -70,6 +70,12 @@ def test_temperatures(lib, t):
     assert b"temperature" in lib.cd_last_error()
 
 
+@pytest.mark.parametrize("t", [3e-39, 3.5e-39, 4.2e-39])
+def test_temperatures_whose_inverse_in_bits_overflows(lib, t):
+    # 1 / t is finite, log2(e) / t is not: every difference of logits would be taken times infinity.
+    test_temperatures(lib, t)
+
+
 def test_distillation_squares_the_temperature(lib):
     assert distill(lib, temperature=1e30) == INVALID
 
