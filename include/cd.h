@@ -436,6 +436,7 @@ cd_status cd_token_logprobs_backward(int64_t B, int64_t T, int64_t V, const void
  *   loss = temperature^2 sum_k q_k (log q_k - log p[id_k]),
  * q = the softmax of teacher_logit / temperature over the row's given entries, p that
  * of the student's logits over the whole vocabulary.
+ * Checks as above, and temperature^2 neither infinite nor below the normal numbers.
  *   K                   entries per row, 1 .. CD_DISTILL_MAX_K
  *   teacher_token [B,T,K]   ids; a negative one marks an absent entry.  A row without
  *                       entries (or with teacher logits of -inf only) has loss 0 and

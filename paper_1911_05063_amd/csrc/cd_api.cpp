@@ -545,7 +545,8 @@ static cd_status check_distill(int64_t B, int64_t T, int64_t V, int K, cd_dtype 
 {
     const cd_status s = check_logits(B, T, V, dtype, stride_b, stride_t, temperature);
     if (s != CD_OK) return s;
-    if (!std::isfinite(temperature * temperature)) return invalid("temperature^2 must be finite");
+    const float t2 = temperature * temperature;
+    if (!std::isnormal(t2)) return invalid("temperature^2 must be finite and not vanish");
     if (K < 1 || K > CD_DISTILL_MAX_K) return invalid("K must be in [1, CD_DISTILL_MAX_K]");
     if (!known_dtype(teacher_dtype)) return invalid("unknown teacher_dtype");
     return CD_OK;

@@ -80,6 +80,15 @@ def test_distillation_squares_the_temperature(lib):
     assert distill(lib, temperature=1e30) == INVALID
 
 
+@pytest.mark.parametrize("t", [1e-30, 1e-20])
+def test_distillation_does_not_lose_the_squared_temperature(lib, t):
+    # The loss would be 0 (or NaN where it is infinite) whatever the logits.
+    assert distill(lib, temperature=t) == INVALID
+    assert b"temperature^2" in lib.cd_last_error()
+    assert distill(lib, temperature=t, loss=None) == INVALID
+    assert distill(lib, temperature=2e-19, loss=None) == INVALID and b"NULL" in lib.cd_last_error()
+
+
 @pytest.mark.parametrize("bad", BAD_ROWS + [dict(K=0), dict(K=257), dict(logits=None), dict(ids=None),
                                             dict(t=None), dict(loss=None), dict(tdtype=7),
                                             dict(saved=ctypes.c_void_p(0x1008))])
