@@ -49,9 +49,12 @@ constexpr int64_t kChunkBytes = int64_t(512) << 20;
 // Rows that are split.  Up to here the weights' 2 D V elements are most of the work: 40 rows of
 // 2048 against 40000 take 224 us instead of 201.
 constexpr int64_t kSplitRows = 256;
-// A product of so few k is bound by its result, which is written past the caches (gradients of 16
-// rows of 2048 against 100000 345 -> 292 us, of 100 rows, k = 200, 496 -> 462; 200 rows of
-// 1024 against 65536, k = 400, are even, 1000 rows of 1000 against 50000 lose: 424 -> 441).
+// A product of so few k is bound by its result, which is written past the caches where they would not
+// keep it (gradients of 16 rows of 2048 against 100000 345 -> 292 us, of 100 rows, k = 200,
+// 496 -> 462; 200 rows of 1024 against 65536, k = 400, are even, 1000 rows of 1000 against 50000
+// lose: 424 -> 441).  Up to 128 MB it may be read from the caches next (gradient of 16 rows of 1024
+// against 65536 106 us in the caches and 109 past them, of 100 rows of 2048 against 16384 113 and
+// 115; the update that reads them next is even).
 constexpr int64_t kStreamK = 256;
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
@@ -397,6 +400,7 @@ struct MulArgs {
     uint32_t tiles_m, tiles_n;
     void *out;              // [M, ld] 16-bit, or null
     int64_t ld;
+    bool stream;            // `out` is written past the caches
     const float *scale;     // scale[1] multiplies what is written to `out`, or null
     float *part;            // [parts, M, N] float32
 };
@@ -454,7 +458,7 @@ __global__ __launch_bounds__(Waves<kTile>::kM *Waves<kTile>::kN * 64, 2) void mu
             }
         };
         // (Two loops: were they one, the compiler would make the two kinds of stores one.)
-        if (a.K <= kStreamK) store(std::true_type{});
+        if (a.stream) store(std::true_type{});
         else store(std::false_type{});
         return;
     }
@@ -528,6 +532,11 @@ MulPlan plan_mul(int64_t M, int64_t N, int64_t K)
     p.part_k = up((K + parts - 1) / parts, kStepK);
     p.parts = static_cast<int>((K + p.part_k - 1) / p.part_k);
     return p;
+}
+
+bool stream_out(int64_t M, int64_t N, int64_t K)
+{
+    return K <= kStreamK && M * N * 2 > kCacheBytes / 2;
 }
 
 bool pack_hidden(const Head &x)
@@ -745,7 +754,8 @@ hipError_t backward(const Head &x, const int32_t *tokens, float temperature, con
             const bool direct = one && !chunks, first = one && chunks && v0 == 0;
             multiply<E, false>(dxo, wc, p,
                                {all, x.D, k, p.part_k, p.tiles_m, p.tiles_n,
-                                direct ? g_hidden : nullptr, x.D, scale, first ? sum : part},
+                                direct ? g_hidden : nullptr, x.D, stream_out(all, x.D, k), scale,
+                                first ? sum : part},
                                stream);
             if (!direct && !first)
                 add_parts<E>(l.rows * x.D, l.copies, p.parts, part, sum, v0 > 0,
@@ -756,7 +766,8 @@ hipError_t backward(const Head &x, const int32_t *tokens, float temperature, con
             E *out = g_weight + v0 * x.D;
             multiply<E, true>(dxo, h, p,
                               {cols, x.D, all, p.part_k, p.tiles_m, p.tiles_n,
-                               p.parts == 1 ? out : nullptr, x.D, scale, part},
+                               p.parts == 1 ? out : nullptr, x.D, stream_out(cols, x.D, all),
+                               scale, part},
                               stream);
             if (p.parts > 1)
                 add_parts<E>(cols * x.D, 1, p.parts, part, nullptr, false, out, scale, stream);
