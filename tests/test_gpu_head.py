@@ -335,3 +335,64 @@ def test_a_float16_gradient_that_is_not_finite_stays_in_its_row(big):
     got = grad(gl)
     rest = torch.arange(40, device="cuda") != 11
     assert torch.equal(got[rest], want[rest]) and not torch.isfinite(got[11]).any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [1, 16, 33, 128])
+@pytest.mark.parametrize("D,V", [(64, 700), (192, 1000), (1088, 400), (2048, 320)])
+def test_few_rows_whose_workgroups_start_at_different_k(T, D, V, dtype):
+    # One row of tiles, D a multiple of 64: of 1, 3, 17 and 32 steps of k each of the (up to 8)
+    # tiles of the vocabulary begins at another and goes round.
+    rng = np.random.default_rng(T + 31 * D + 1009 * V)
+    h, w, tokens = make(rng, T, D, V, dtype)
+    if T > 1:
+        tokens[0], tokens[1] = V - 1, V
+    check(h, w, tokens, dtype, [1.0, 0.7, 2.0][T % 3], 1.0 if dtype == "bf16" else 300.0)
+
+
+@pytest.mark.parametrize("T,dtype", [(3, "bf16"), (70, "f16")])
+def test_few_rows_of_weights_that_go_past_the_caches(T, dtype):
+    rng = np.random.default_rng(23)
+    D, V = 1024, 65537                          # more than 128 MB, the last tile of one column
+    h, w, tokens = make(rng, T, D, V, dtype)
+    tokens[0], tokens[1], tokens[2] = V - 1, V, -1
+    check(h, w, tokens, dtype, gscale=1.0 if dtype == "bf16" else 300.0)
+
+
+def test_ranges_of_the_vocabulary_over_few_rows():
+    # d/d logits in two parts, and two ranges of 524288 columns, the last short.
+    T, D, V = 200, 16, 600001
+    g = torch.Generator(device="cuda").manual_seed(24)
+    h = torch.randn(T, D, device="cuda", generator=g).bfloat16().requires_grad_()
+    w = torch.randn(V, D, device="cuda", generator=g).bfloat16().requires_grad_()
+    tokens = torch.randint(-1, V, (T,), device="cuda", dtype=torch.int32, generator=g)
+    tokens[:3] = torch.tensor([V - 1, 524287, 524288])
+    lp, _ = cd.head_logprobs(h, w, tokens)
+    g0 = torch.rand(T, device="cuda", generator=g)
+    gh, gw = torch.autograd.grad([lp], [h, w], [g0])
+    hf, wf = h.detach().float(), w.detach().float()
+    logp = torch.log_softmax(hf @ wf.t(), 1)
+    at, used = tokens.clamp_min(0).long()[:, None], tokens >= 0
+    assert (lp - torch.where(used, logp.gather(1, at)[:, 0], 0)).abs().max() < 1e-4
+    d = -logp.exp_() * (g0 * used)[:, None]
+    d.scatter_add_(1, at, (g0 * used)[:, None])
+    # The result rounded to 2^-8; d in two parts, and float32 logits of about 20 in both.
+    for got, ref, size in ((gh, d @ wf, d.abs() @ wf.abs()), (gw, d.t() @ hf, d.abs().t() @ hf.abs())):
+        assert ((got.float() - ref).abs() <= 1.01 * 2.0 ** -8 * ref.abs() + 1e-4 * size + 1e-7).all()
+
+
+def test_large_steps_give_the_same_bits():
+    # Large tiles in all products, sums over ranges of the vocabulary and over parts.
+    for T, D, V, dtype in ((8192, 512, 65536, "bf16"), (3001, 1000, 10007, "f16")):
+        g = torch.Generator(device="cuda").manual_seed(25)
+        h = torch.randn(T, D, device="cuda", generator=g).to(DTYPES[dtype]).requires_grad_()
+        w = (torch.randn(V, D, device="cuda", generator=g) / 16).to(DTYPES[dtype]).requires_grad_()
+        tokens = torch.randint(-1, V, (T,), device="cuda", dtype=torch.int32, generator=g)
+
+        def step():
+            out = cd.head_logprobs(h, w, tokens)
+            return out + torch.autograd.grad(out[0].sum() + out[1].sum(), [h, w])
+
+        first = step()
+        for _ in range(5):
+            assert all(torch.equal(a, b) for a, b in zip(step(), first))
