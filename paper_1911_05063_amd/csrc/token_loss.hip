@@ -664,7 +664,8 @@ __global__ __launch_bounds__(kPer > kWaves ? kPer * 64 : kThreads) void rows_ker
                 if (wave == 0) {
                     uint64_t some = sort_keys(meet.keys[lane], lane);
                     if (a.k > 32) some = merge_keys(some, sort_keys(meet.keys[64 + lane], lane), lane);
-                    if (lane == 0) meet.last = key_lane(some, a.k - 1);
+                    const uint64_t last = key_lane(some, a.k - 1);     // (by all lanes, as it is of one)
+                    if (lane == 0) meet.last = last;
                 }
                 __syncthreads();
                 Best found = candidates(x, a.V, v0, v1, per_group, groups, ngroups, meet.last, a.k,
