@@ -2,10 +2,15 @@
 // and an operation between lanes is where they meet.  The kernels' memory accesses are then the
 // process's own, and one that leaves its buffer meets an unmapped page beside it.
 //
+// Loads straight to LDS arrive as late as a wait allows (or, lanes::early, at once), and waves run one
+// after another from barrier to barrier, in either order (lanes::backwards): a missing wait or
+// barrier gives wrong results.
+//
 // Lanes that wait at the same operation take part in it, as if the others were masked off: right
 // where the lanes that read each other (a wave, or 16 lanes) go the same way.
 #pragma once
 
+#include <setjmp.h>
 #include <ucontext.h>
 
 #include <algorithm>
@@ -29,6 +34,12 @@ inline hipError_t hipGetLastError() { return hipSuccess; }
 #define __shared__ static
 #define __forceinline__ inline
 #define __launch_bounds__(...)
+#define address_space(n)
+
+struct dim3 {
+    unsigned x = 1, y = 1, z = 1;
+    dim3(unsigned x, unsigned y = 1, unsigned z = 1) : x(x), y(y), z(z) {}
+};
 
 namespace lanes {
 
@@ -39,38 +50,61 @@ namespace lanes {
     abort();
 }
 
-enum Kind { kFence, kBallot, kDpp, kSwap16, kSwap32, kReadLane, kReadFirst, kShuffle, kBarrier, kDone, kRun };
+enum Kind { kFence, kBallot, kDpp, kSwap16, kSwap32, kReadLane, kReadFirst, kShuffle, kTranspose, kMatrix, kBarrier, kDone, kRun };
 
 struct Lane {
-    ucontext_t context;
+    ucontext_t context;     // its start
+    jmp_buf here;           // where it waits
+    bool started;
     unsigned id;
     Kind kind;
     int control;        // of which lanes that meet have the same
     unsigned from;      // lane that is read
     uint32_t in, in2, out, out2;
+    int16_t part[4];    // kTranspose: read, and result
+    float a[8], b[8];   // kMatrix: a row of each operand
+    float c[4];
+    struct Load {
+        char *to;
+        char bytes[16];
+    };
+    std::vector<Load> loads;    // on their way to LDS
 };
+inline bool early, backwards;
 
 struct Index {
     unsigned x, y, z;
 };
 inline Index block, grid, dim;
 inline Lane *lane_now;
-inline ucontext_t scheduler;
+inline jmp_buf scheduler;
 inline std::function<void()> body;
 
-inline void enter()
+__attribute__((noinline)) inline void resume(Lane *l)
 {
-    body();
-    lane_now->kind = kDone;
-    swapcontext(&lane_now->context, &scheduler);
+    lane_now = l;
+    if (_setjmp(scheduler) != 0) return;
+    if (l->started) _longjmp(l->here, 1);
+    l->started = true;
+    setcontext(&l->context);
+}
+
+__attribute__((noinline)) inline void pause()
+{
+    if (_setjmp(lane_now->here) == 0) _longjmp(scheduler, 1);
 }
 
 inline void wait(Kind kind, int control = 0)
 {
-    Lane *me = lane_now;
-    me->kind = kind;
-    me->control = control;
-    swapcontext(&me->context, &scheduler);
+    lane_now->kind = kind;
+    lane_now->control = control;
+    pause();
+}
+
+inline void enter()
+{
+    body();
+    wait(kDone);
 }
 
 // The operation that the lanes `some` of a wave wait at.
@@ -113,30 +147,66 @@ inline void join(Lane *wave, uint64_t some)
             if (!has(me.from)) stop("a value is read of a lane that is elsewhere");
             me.out = read(me.from);
             break;
+        case kTranspose:
+        case kMatrix: break;
         case kShuffle: me.out = read(row + me.from); break;
         case kReadFirst: me.out = read(static_cast<unsigned>(__builtin_ctzll(some))); break;
         default: break;
         }
     }
+    // 16 lanes' 4 elements each, 4 rows of 16: a lane gets a column.
+    const Kind kind = wave[__builtin_ctzll(some)].kind;
+    if (kind == kTranspose) {
+        int16_t got[64][4];
+        for (unsigned l = 0; l < 64; ++l)
+            for (unsigned j = 0; j < 4; ++j) got[l][j] = wave[(l & ~15u) + j * 4 + (l & 15) / 4].part[l & 3];
+        for (unsigned l = 0; l < 64; ++l) memcpy(wave[l].part, got[l], 8);
+    }
+    // Lane l has row l & 15 of each operand at k = (l >> 4) * 8 .., and result rows (l >> 4) * 4 ..
+    // of column l & 15.
+    if (kind == kMatrix) {
+        float a[16][32], b[32][16];
+        for (unsigned l = 0; l < 64; ++l)
+            for (unsigned k = 0; k < 8; ++k) {
+                a[l & 15][l / 16 * 8 + k] = wave[l].a[k];
+                b[l / 16 * 8 + k][l & 15] = wave[l].b[k];
+            }
+        for (unsigned row = 0; row < 16; ++row) {
+            float c[16] = {};
+            for (unsigned k = 0; k < 32; ++k)
+                for (unsigned n = 0; n < 16; ++n) c[n] += a[row][k] * b[k][n];
+            for (unsigned n = 0; n < 16; ++n) wave[row / 4 * 16 + n].c[row % 4] += c[n];
+        }
+    }
+    if ((kind == kTranspose || kind == kMatrix) && some != ~uint64_t(0)) stop("part of a wave at a matrix");
     for (unsigned l = 0; l < 64; ++l)
         if (has(l)) wave[l].kind = kRun;
 }
 
+inline void arrive(Lane &l, size_t pending)
+{
+    const size_t n = l.loads.size() > pending ? l.loads.size() - pending : 0;
+    for (size_t i = 0; i < n; ++i) memcpy(l.loads[i].to, l.loads[i].bytes, 16);
+    l.loads.erase(l.loads.begin(), l.loads.begin() + n);
+}
+
 template <typename F>
-void launch(unsigned blocks, unsigned threads, F &&f)
+void launch(dim3 blocks, unsigned threads, F &&f)
 {
     static std::vector<Lane> lanes(1024);
     static std::vector<char> stacks(size_t(1024) << 16);
     if (threads % 64 != 0 || threads > 1024) stop("a workgroup of part of a wave, or of more than 1024");
     body = f;
-    grid = {blocks, 1, 1};
+    grid = {blocks.x, blocks.y, 1};
     dim = {threads, 1, 1};
-    for (unsigned b = 0; b < blocks; ++b) {
-        block = {b, 0, 0};
+    for (unsigned b = 0; b < blocks.x * blocks.y; ++b) {
+        block = {b % blocks.x, b / blocks.x, 0};
         for (unsigned i = 0; i < threads; ++i) {
             Lane &l = lanes[i];
             l.id = i;
             l.kind = kRun;
+            l.started = false;
+            l.loads.clear();
             getcontext(&l.context);
             l.context.uc_stack.ss_sp = stacks.data() + (size_t(i) << 16);
             l.context.uc_stack.ss_size = size_t(1) << 16;
@@ -146,14 +216,11 @@ void launch(unsigned blocks, unsigned threads, F &&f)
         for (;;) {
             unsigned done = 0, waiting = 0;
             for (unsigned w = 0; w < threads; w += 64) {
-                Lane *wave = &lanes[w];
+                Lane *wave = &lanes[backwards ? threads - 64 - w : w];
                 for (;;) {
                     int first = -1;
                     for (int i = 0; i < 64; ++i) {
-                        if (wave[i].kind == kRun) {
-                            lane_now = &wave[i];
-                            swapcontext(&scheduler, &wave[i].context);
-                        }
+                        if (wave[i].kind == kRun) resume(&wave[i]);
                         if (first < 0 && wave[i].kind < kBarrier) first = i;
                     }
                     if (first < 0) break;
@@ -198,6 +265,38 @@ inline uint64_t ballot(bool x, int line)
     return static_cast<uint64_t>(lane_now->out2) << 32 | lane_now->out;
 }
 inline uint32_t below(uint64_t mask) { return __builtin_popcountll(mask & ((uint64_t(1) << (lane_now->id & 63)) - 1)); }
+template <typename V>
+V transpose(const V *p)
+{
+    memcpy(lane_now->part, p, 8);
+    wait(kTranspose);
+    V v;
+    memcpy(&v, lane_now->part, 8);
+    return v;
+}
+template <typename V, typename C>
+C matrix(const V &a, const V &b, const C &c)
+{
+    for (int i = 0; i < 8; ++i) {
+        lane_now->a[i] = static_cast<float>(a[i]);
+        lane_now->b[i] = static_cast<float>(b[i]);
+    }
+    memcpy(lane_now->c, &c, 16);
+    wait(kMatrix);
+    C out;
+    memcpy(&out, lane_now->c, 16);
+    return out;
+}
+inline void load(const void *from, void *lds, unsigned offset)
+{
+    Lane::Load l;
+    l.to = static_cast<char *>(lds) + (lane_now->id & 63) * 16;
+    memcpy(l.bytes, static_cast<const char *>(from) + offset, 16);
+    lane_now->loads.push_back(l);
+    if (early) arrive(*lane_now, 0);
+}
+inline void waitcnt(unsigned n) { arrive(*lane_now, (n & 15) | (n >> 14 & 3) << 4); }
+
 inline Index thread() { return {lane_now->id, 0, 0}; }
 
 template <typename T>
@@ -229,6 +328,16 @@ T fetch(T *p, T v, T (*f)(T, T))
 #define __builtin_amdgcn_mbcnt_lo(mask, n) ((n) + lanes::below(mask))
 #define __builtin_amdgcn_mbcnt_hi(mask, n) ((n) + lanes::below(static_cast<uint64_t>(mask) << 32))
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
+#define __builtin_amdgcn_make_buffer_rsrc(p, stride, size, flags) (p)
+#define __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, size, offset, add, at, cache) \
+    lanes::load(from, lds, static_cast<unsigned>(offset))
+#define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) lanes::transpose(p)
+#define __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, x, y, z) lanes::matrix(a, b, c)
+#define __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, x, y, z) lanes::matrix(a, b, c)
+#define __builtin_amdgcn_s_waitcnt(n) lanes::waitcnt(n)
+#define __builtin_amdgcn_s_barrier() lanes::wait(lanes::kBarrier)
+#define __builtin_amdgcn_sched_barrier(x) (void)0
+#define __builtin_amdgcn_sched_group_barrier(x, y, z) (void)0
 #define __builtin_nontemporal_load(p) (*(p))
 #define __builtin_nontemporal_store(v, p) (void)(*(p) = (v))
 
