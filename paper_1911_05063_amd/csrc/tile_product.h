@@ -264,14 +264,13 @@ struct TileProduct {
     // everywhere.  At step s the buffers of s - 1 (m or n adjacent) are read no more and take
     // the loads of s + 3; at step s + 1 those of s take s + 4's, and what is staged 64 k at a
     // time, all read by then, takes s + 4's and s + 5's.  So every load has two steps' time.
-    // (The buffers written and those read transposed are different ones, and `restrict` says
-    // so: otherwise the compiler waits for the loads before every transposed read.)
-    static __device__ __forceinline__ void two_steps(
-        A &sa, B &sb, int s, int steps, int wave, char *__restrict__ a_s3, char *__restrict__ a_s4,
-        char *__restrict__ b_s3, char *__restrict__ b_s4, const char *__restrict__ a_s1,
-        const char *__restrict__ a_s2, const char *__restrict__ b_s1,
-        const char *__restrict__ b_s2, const int *places_a, const int *places_b, Frags &f,
-        f32x4 (&acc)[kM][kN])
+    static __device__ __forceinline__ void two_steps(A &sa, B &sb, int s, int steps, int wave,
+                                                     char *a_s3, char *a_s4, char *b_s3,
+                                                     char *b_s4, const char *a_s1,
+                                                     const char *a_s2, const char *b_s1,
+                                                     const char *b_s2, const int *places_a,
+                                                     const int *places_b, Frags &f,
+                                                     f32x4 (&acc)[kM][kN])
     {
         if (kEach > 0) {
             if (s + 2 < steps) meet<kEach + kOther, false>();
@@ -291,6 +290,32 @@ struct TileProduct {
             if (kAcrossB) sb.load(b_s4, wave);
         }
         half_step(1, a_s2, b_s2, places_a, places_b, f, acc);   // (at the end: of what is not used)
+    }
+
+    // Different buffers are told apart by `restrict`: otherwise the compiler has every read wait for all
+    // loads to LDS.  Where both k are adjacent, each buffer is in its place again after four steps (s
+    // a multiple of 4); else the four of m or n adjacent are all different within two.
+    static __device__ __forceinline__ void four_steps(A &sa, B &sb, int s, int steps, int wave,
+                                                      char *__restrict__ a0, char *__restrict__ a1,
+                                                      char *__restrict__ b0, char *__restrict__ b1,
+                                                      const int *places_a, const int *places_b,
+                                                      Frags &f, f32x4 (&acc)[kM][kN])
+    {
+        two_steps(sa, sb, s, steps, wave, a1, a0, b1, b0, a0, a1, b0, b1, places_a, places_b, f, acc);
+        if (s + 2 < steps)
+            two_steps(sa, sb, s + 2, steps, wave, a0, a1, b0, b1, a1, a0, b1, b0, places_a, places_b, f,
+                      acc);
+    }
+    // (With k adjacent the buffer of step s + 1 is that of s + 4.)
+    static __device__ __forceinline__ void two_steps_across(
+        A &sa, B &sb, int s, int steps, int wave, char *__restrict__ a_s3, char *__restrict__ a_s4,
+        char *__restrict__ b_s3, char *__restrict__ b_s4, const char *__restrict__ a_s1,
+        const char *__restrict__ a_s2, const char *__restrict__ b_s1,
+        const char *__restrict__ b_s2, const int *places_a, const int *places_b, Frags &f,
+        f32x4 (&acc)[kM][kN])
+    {
+        two_steps(sa, sb, s, steps, wave, a_s3, a_s4, b_s3, b_s4, kAcrossA ? a_s1 : a_s4, a_s2,
+                  kAcrossB ? b_s1 : b_s4, b_s2, places_a, places_b, f, acc);
     }
 
     // acc[i][j][r] = C[m0 + wm + i * 16 + (lane & 15)][n0 + wn + j * 16 + (lane >> 4) * 4 + r]
@@ -358,11 +383,18 @@ struct TileProduct {
         for (int j = 0; j < kN; ++j) f.b[0][j] = B::read(lds_b, places_b, j, 0);
 #pragma unroll
         for (int i = 0; i < kM; ++i) f.a[0][i] = A::read(lds_a, places_a, i, 0);
-        for (int s = 0; s < steps; s += 2)
-            two_steps(sa, sb, s, steps, wave, lds_a + A::buffer(s + 3),
-                      lds_a + A::buffer(s + 4), lds_b + B::buffer(s + 3),
-                      lds_b + B::buffer(s + 4), lds_a + A::buffer(s + 1), lds_a + A::buffer(s + 2),
-                      lds_b + B::buffer(s + 1), lds_b + B::buffer(s + 2), places_a, places_b, f, acc);
+        if constexpr (kEach == 0) {
+            for (int s = 0; s < steps; s += 4)
+                four_steps(sa, sb, s, steps, wave, lds_a, lds_a + A::kBytes, lds_b, lds_b + B::kBytes,
+                           places_a, places_b, f, acc);
+        } else {
+            for (int s = 0; s < steps; s += 2)
+                two_steps_across(sa, sb, s, steps, wave, lds_a + A::buffer(s + 3),
+                                 lds_a + A::buffer(s + 4), lds_b + B::buffer(s + 3),
+                                 lds_b + B::buffer(s + 4), lds_a + A::buffer(s + 1),
+                                 lds_a + A::buffer(s + 2), lds_b + B::buffer(s + 1),
+                                 lds_b + B::buffer(s + 2), places_a, places_b, f, acc);
+        }
     }
 
     // A wave's results as 16-bit rows of 64 columns, by way of LDS: from four columns of 16 rows
