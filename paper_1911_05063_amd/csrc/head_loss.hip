@@ -57,6 +57,11 @@ constexpr int64_t kSplitRows = 256;
 // 115; the update that reads them next is even).
 constexpr int64_t kStreamK = 256;
 
+// Rows of a workgroup that looks for the scale of float16, and the most workgroups (131072 rows 12 us in
+// two launches, by one workgroup 110; 3001 rows 3 us by one).
+constexpr int64_t kScaleRows = 4096;
+constexpr int kScaleParts = 62;
+
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 size_t up256(size_t a) { return (a + 255) / 256 * 256; }
 
@@ -255,35 +260,48 @@ struct HeadRow {
     int32_t pad;
 };
 
-// The power of 2 that takes the largest possible |dx| to about 2^14 (float16), over what
-// head_rows_kernel takes: a row without a token or a gradient may come with any g.  Nor do rows count
-// whose g is not finite: their d/d hidden is not at any scale, the other rows' is.  One workgroup.
+// The power of 2 that takes the largest possible |dx|, `most`, to about 2^14 (float16).
+__device__ __forceinline__ void set_scale(float most, float *scale)
+{
+    int e = 0;
+    if (most > 0.0f) e = 14 - ilogbf(most);
+    e = e > 100 ? 100 : e < -100 ? -100 : e;
+    scale[0] = ldexpf(1.0f, e);
+    scale[1] = ldexpf(1.0f, -e);
+}
+
+// That of all rows by one workgroup, or (several) the largest possible |dx| of each workgroup's.  Rows
+// count as head_rows_kernel takes them: one without a token or a gradient may come with any g.
+// Nor do rows count whose g is not finite: their d/d hidden is not at any scale, the other rows' is.
 __global__ __launch_bounds__(1024) void scale_kernel(int32_t T, int32_t V, float lnv,
                                                      float inv_temperature, const int32_t *tokens,
                                                      const ScoreRow *saved, const float *g_logprob,
-                                                     const float *g_entropy, float *scale)
+                                                     const float *g_entropy, float *parts,
+                                                     float *scale)
 {
     __shared__ float part[16];
     float most = 0.0f;
-    for (int32_t i = threadIdx.x; i < T; i += 1024) {
+    for (int64_t i = blockIdx.x * 1024 + threadIdx.x; i < T; i += gridDim.x * 1024) {
+        // (all asked for at once, used or not)
         const int32_t t = tokens[i];
-        if (t < 0 || saved[i].m == -INFINITY) continue;
-        float g = g_logprob && t < V ? fabsf(g_logprob[i]) : 0.0f;
-        if (g_entropy) g += fabsf(g_entropy[i]) * (lnv + 1.0f);
-        g *= inv_temperature;
-        if (g < INFINITY) most = fmaxf(most, g);
+        const float m = saved[i].m;
+        const float gl = g_logprob ? fabsf(g_logprob[i]) : 0.0f;
+        const float ge = g_entropy ? fabsf(g_entropy[i]) : 0.0f;
+        const float g = ((t < V ? gl : 0.0f) + ge * (lnv + 1.0f)) * inv_temperature;
+        if (t >= 0 && m != -INFINITY && g < INFINITY) most = fmaxf(most, g);
     }
     most = group_max<64>(most);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 16; ++i) most = fmaxf(most, part[i]);
-        int e = 0;
-        if (most > 0.0f) e = 14 - ilogbf(most);
-        e = e > 100 ? 100 : e < -100 ? -100 : e;
-        scale[0] = ldexpf(1.0f, e);
-        scale[1] = ldexpf(1.0f, -e);
-    }
+    if (threadIdx.x != 0) return;
+    for (int i = 1; i < 16; ++i) most = fmaxf(most, part[i]);
+    if (gridDim.x == 1) set_scale(most, scale);
+    else parts[blockIdx.x] = most;
+}
+__global__ __launch_bounds__(64) void join_scale_kernel(int n, const float *parts, float *scale)
+{
+    const float most = group_max<64>(static_cast<int>(threadIdx.x) < n ? parts[threadIdx.x] : 0.0f);
+    if (threadIdx.x == 0) set_scale(most, scale);
 }
 
 __global__ __launch_bounds__(kRowThreads) void head_rows_kernel(
@@ -611,7 +629,7 @@ HeadLayout layout_of(const Head &x, bool backward)
     const int64_t all = l.rows * l.copies, rows = dx_rows(all);
     const int64_t most = std::max<int64_t>(kChunkBytes / (rows * 2), 1024);
     l.chunk = std::min(up(x.V, kBig), most / kBig * kBig);
-    l.scale = take(2 * sizeof(float));
+    l.scale = take((2 + kScaleParts) * sizeof(float));
     l.head_rows = take(static_cast<size_t>(rows) * sizeof(HeadRow));
     l.dx = take(static_cast<size_t>(rows) * l.chunk * 2);
     // Parts of d/dh and of d/dw share their place: one is summed up before the other starts.
@@ -718,10 +736,13 @@ hipError_t backward(const Head &x, const int32_t *tokens, float temperature, con
     float *scale = nullptr;
     if (x.dtype == CD_F16) {
         scale = at<float>(ws, l.scale);
-        scale_kernel<<<1, 1024, 0, stream>>>(static_cast<int32_t>(l.rows),
-                                             static_cast<int32_t>(x.V),
-                                             logf(static_cast<float>(x.V)), inv, tokens, saved,
-                                             g_logprob, g_entropy, scale);
+        const int parts = static_cast<int>(
+            std::min<int64_t>((l.rows + kScaleRows - 1) / kScaleRows, kScaleParts));
+        scale_kernel<<<parts, 1024, 0, stream>>>(static_cast<int32_t>(l.rows),
+                                                 static_cast<int32_t>(x.V),
+                                                 logf(static_cast<float>(x.V)), inv, tokens, saved,
+                                                 g_logprob, g_entropy, scale + 2, scale);
+        if (parts > 1) join_scale_kernel<<<1, 64, 0, stream>>>(parts, scale + 2, scale);
     }
     HeadRow *head_rows = at<HeadRow>(ws, l.head_rows);
     head_rows_kernel<<<static_cast<unsigned>(up(rows, kRowThreads) / kRowThreads), kRowThreads, 0,

@@ -294,7 +294,7 @@ def test_what_lies_between_the_rows_of_the_weights_is_not_used(T, D, V, ld, arou
             assert all(torch.equal(a, b) for a, b in zip(some, want))
 
 
-@pytest.mark.parametrize("T", [40, 300])
+@pytest.mark.parametrize("T", [40, 300, 9001])
 @pytest.mark.parametrize("big", [1e6, 1e30, float("inf"), float("nan")])
 def test_float16_gradients_of_rows_that_take_none_do_not_scale_the_others(T, big):
     rng = np.random.default_rng(21)

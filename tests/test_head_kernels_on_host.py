@@ -89,3 +89,8 @@ def test_head(lib, B, T, D, V, dtype, gap, at_end, early, backwards):
 def test_tiles_of_256(lib, T, D, V, early, backwards):
     # In turn: logits (some workgroups take one tile, in 160 in all) and d/d logits, d/d weights, d/d hidden.
     in_child(run, lib, 1, T, D, V, BF16, 8 if D % 8 == 0 else 0, True, early, backwards)
+
+
+def test_scale_of_many_rows(lib):
+    # Several workgroups look for the scale of float16 gradients.
+    in_child(run, lib, 1, 9000, 8, 20, F16, 0, True, 0, 0)
