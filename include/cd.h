@@ -375,11 +375,12 @@ cd_status cd_emd_backward(int64_t B, int64_t N, int64_t M, const float *X, const
  *    adjacent; rows need only the alignment of an element.  Per-row arrays are
  *    contiguous [B, T], gradients contiguous [B, T, V] in the logits' type.
  *  - temperature > 0 divides the logits.  With z = logits / temperature, p is the
- *    softmax of z.  Everything is held in float32; a gradient is rounded once.
+ *    softmax of z.  Everything is held in float32; a gradient is rounded once
+ *    (cd_head_logprobs_backward rounds d/d logits as well, see there).
  *  - A logit of -inf, or so low that its weight vanishes, has p = 0, adds nothing
- *    to an entropy and has a gradient of 0.  In a row of -inf only, log
- *    probabilities are -inf, the entropy is 0 and the gradient is 0.  NaN or +inf
- *    make the row's results NaN.
+ *    to an entropy and has a gradient of 0 (that of its own log probability apart).
+ *    In a row of -inf only, log probabilities are -inf, the entropy is 0 and the
+ *    gradient is 0.  NaN or +inf make the row's results NaN.
  *  - Checks (else CD_ERR_INVALID_ARG, nothing launched): B, T >= 0, B * T < 2^31,
  *    1 <= V < 2^31, strides >= 0, a known dtype, temperature positive and finite
  *    (and log2(e) / temperature finite).  B * T == 0 is a no-op.
@@ -407,7 +408,7 @@ size_t cd_token_workspace_bytes(int64_t B, int64_t T, int64_t V, cd_dtype dtype,
  *   entropy [B,T]       -sum p log p (nats)
  *   top_logprob, top_token [B,T,top]   the largest logits' log probabilities and ids,
  *                       descending, equal logits by the lowest id (-0 equals 0); NULL iff
- *                       top = 0.  Unspecified order in a row with a NaN.
+ *                       top = 0.  In a row with a NaN any tokens, or -1.
  *   saved               CD_TOKEN_SAVED_BYTES bytes per row for the backward, 16-byte
  *                       aligned, or NULL
  *   ws, ws_bytes        cd_token_workspace_bytes, 256-byte aligned
@@ -493,9 +494,15 @@ cd_status cd_head_logprobs_forward(int64_t B, int64_t T, int64_t D, int64_t V, c
 /*
  * Gradients of sum g_logprob logprob + g_entropy entropy: g_hidden contiguous [B,T,D], g_weight
  * contiguous [V,D], of dtype, 16-byte aligned, fully overwritten; either may be NULL (not
- * computed), and so may g_logprob and g_entropy (zero).  d/d logits is rounded to dtype
- * (scaled by a power of 2 where that is CD_F16) before its products with weight and hidden,
- * which are summed up in float32.  B * T == 0 leaves g_weight as it is.
+ * computed), and so may g_logprob and g_entropy (zero).  What they hold for a row that takes no
+ * gradient has no influence on the others'.  B * T == 0 leaves g_weight as it is.
+ *
+ * d/d logits is rounded to dtype before its products with weight and hidden, which are summed
+ * up in float32: once for each element above 256 rows (the gradients' error is then about
+ * 1.45 times that of float32 d/d logits), and up to 256 rows with the rest of the rounding kept
+ * beside it, so that the gradients' own rounding is what is left.  Where dtype is CD_F16 it is
+ * scaled before by one power of 2, which takes the largest possible element of all rows whose
+ * g_logprob and g_entropy are finite to about 2^14.
  */
 cd_status cd_head_logprobs_backward(int64_t B, int64_t T, int64_t D, int64_t V, const void *hidden,
                                     const void *weight, cd_dtype dtype, int64_t stride_b,

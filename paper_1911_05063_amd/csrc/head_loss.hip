@@ -7,22 +7,22 @@
 //
 // Backward: with dx = d/dx of token_loss.hip,
 //     d/dh = dx w,   d/dw = dx^T h.
-// The logits are computed again (the same products; over few rows in another order), so
-// 6 T D V operations become 8.  dx is rounded to the operands' type for the matrix cores,
-// like the operands themselves; in float16 it is scaled by a power of 2 first, so that the
-// largest possible element is about 2^14 and small ones do not vanish.  The rounding adds as
-// much to the results' error as their own rounding does (0.0024 instead of 0.0017, relative,
-// in bfloat16).  Over few rows the errors do not average: up to kSplitRows rows, dx is
-// held as a rounded part and a second row with the rest, which both go through the products.
-// It is held for a range of the vocabulary at a time (kChunkBytes): d/dw of the range is
-// finished with it, d/dh is summed over ranges, and over parts of a long sum where few tiles
-// would leave CUs idle, in float32 and in a fixed order.
+// The logits are computed again (the same products; over few rows in another order), so 6 T D V
+// operations become 8.  dx is rounded to the operands' type for the matrix cores, like the
+// operands themselves; in float16 it is scaled by a power of 2 first, so that the largest possible
+// element is about 2^14 and small ones do not vanish.  The rounding adds as much to the results'
+// error as their own rounding does (relative: 0.0024 instead of 0.0017 in bfloat16, 3.0e-4 instead
+// of 2.1e-4 in float16).  Over few rows the errors do not average: up to kSplitRows rows, dx is
+// held as a rounded part and a second row with the rest, which both go through the products.  It
+// is held for a range of the vocabulary at a time (kChunkBytes): d/dw of the range is finished
+// with it, d/dh is summed over ranges, and over parts of a long sum where few tiles would leave
+// CUs idle, in float32 and in a fixed order.
 //
 // Bound by the matrix cores' clock under load and the tiles' ends.  8192 rows of 2048 against
-// 65536, bfloat16, 2.2e12 operations a product (TFLOP/s): stats_kernel 1160, dx_kernel 1095,
-// mul_kernel 1300 (d/dh) and 1140 (d/dw), 7.0 ms in all, where a plain library product reaches
-// 1320; the matrix cores are busy in 59, 54 and 59% of all cycles.  16 rows of 2048 against 65536
-// are the weights' 268 MB in 53 us, 5.1 TB/s.
+// 65536, bfloat16, 2.2e12 operations a product (TFLOP/s): stats_kernel 1285, dx_kernel 1165,
+// mul_kernel 1390 (d/dh) and 1210 (d/dw), 7.1 ms in all, where a plain library product reaches
+// 1320; the matrix cores are busy in 63, 55, 63 and 57% of all cycles.  16 rows of 2048 against
+// 65536 are the weights' 268 MB in 53 us, 5.1 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -36,9 +36,9 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kBig = 256, kSmall = 128;         // tiles: 8 waves (2 x 4), 4 waves (2 x 2)
 // Fewer large tiles than this leave too many of the 256 CUs without one (us, large -> small tiles,
-// forward: 128 large tiles 2048 x 1024 against 4096 34 -> 25, 160 against 5120 34.8 -> 34.3, but
-// 192 2048 x 2048 against 6144 54 -> 58, 256 against 8192 59 -> 66).  Large tiles read less
-// from LDS for each product: 12 fragments for 32 products instead of 8 for 16.
+// forward: 128 large tiles 2048 x 1024 against 4096 34 -> 25, 160 against 5120 even, but 192 2048
+// x 2048 against 6144 54 -> 58, 256 against 8192 59 -> 66).  Large tiles read less from LDS for
+// each product: 12 fragments for 32 products instead of 8 for 16.
 constexpr int64_t kFewTiles = 160;
 constexpr unsigned kCus = 256;                  // a workgroup of a large tile each
 constexpr int64_t kWantTiles = 512;             // small tiles wanted, two for each CU
@@ -49,16 +49,16 @@ constexpr int64_t kChunkBytes = int64_t(512) << 20;
 // Rows that are split.  Up to here the weights' 2 D V elements are most of the work: 40 rows of
 // 2048 against 40000 take 224 us instead of 201.
 constexpr int64_t kSplitRows = 256;
-// A product of so few k is bound by its result, which is written past the caches where they would not
-// keep it (gradients of 16 rows of 2048 against 100000 345 -> 292 us, of 100 rows, k = 200,
+// A product of so few k is bound by its result, which is written past the caches where they would
+// not keep it (gradients of 16 rows of 2048 against 100000 345 -> 292 us, of 100 rows, k = 200,
 // 496 -> 462; 200 rows of 1024 against 65536, k = 400, are even, 1000 rows of 1000 against 50000
-// lose: 424 -> 441).  Up to 128 MB it may be read from the caches next (gradient of 16 rows of 1024
-// against 65536 106 us in the caches and 109 past them, of 100 rows of 2048 against 16384 113 and
-// 115; the update that reads them next is even).
+// lose: 424 -> 441).  Up to 128 MB it may be read from the caches next (gradient of 16 rows of
+// 1024 against 65536 106 us in the caches and 109 past them, of 100 rows of 2048 against 16384 113
+// and 115; the update that reads them next is even).
 constexpr int64_t kStreamK = 256;
 
-// Rows of a workgroup that looks for the scale of float16, and the most workgroups (131072 rows 12 us in
-// two launches, by one workgroup 110; 3001 rows 3 us by one).
+// Rows of a workgroup that looks for the scale of float16, and the most workgroups (131072 rows 12
+// us in two launches, by one workgroup 110; 3001 rows 3 us by one).
 constexpr int64_t kScaleRows = 4096;
 constexpr int kScaleParts = 62;
 
@@ -270,9 +270,10 @@ __device__ __forceinline__ void set_scale(float most, float *scale)
     scale[1] = ldexpf(1.0f, -e);
 }
 
-// That of all rows by one workgroup, or (several) the largest possible |dx| of each workgroup's.  Rows
-// count as head_rows_kernel takes them: one without a token or a gradient may come with any g.
-// Nor do rows count whose g is not finite: their d/d hidden is not at any scale, the other rows' is.
+// That of all rows by one workgroup, or (several) the largest possible |dx| of each workgroup's.
+// Rows count as head_rows_kernel takes them: one without a token or a gradient may come with any
+// g. Nor do rows count whose g is not finite: their d/d hidden is not at any scale, the other
+// rows' is.
 __global__ __launch_bounds__(1024) void scale_kernel(int32_t T, int32_t V, float lnv,
                                                      float inv_temperature, const int32_t *tokens,
                                                      const ScoreRow *saved, const float *g_logprob,

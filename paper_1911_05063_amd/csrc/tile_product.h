@@ -22,10 +22,11 @@
 // lanes, and stores are 8 or 16 bytes.
 //
 // What bounds it: a step of 32 k is 32 products of 16 cycles for a wave of a large tile, in between
-// its 12 fragments are read from LDS, and every load has two steps' time.  The loop reaches 1200
-// to 1350 TFLOP/s at the 1.8 to 2.0 GHz that the card holds under this load (8192 x 65536 x
-// 2048, bfloat16; 256 x 256 tiles of 8 waves, one workgroup a CU); bank conflicts are 0.5% of
-// the LDS cycles.  A tile's first loads and its end, 4 to 10 us, overlap with no products.
+// its 12 fragments are read from LDS, and every load has two steps' time.  The kernels reach 1165
+// to 1390 TFLOP/s at the 1.8 to 2.0 GHz that the card holds under this load (8192 x 65536 x
+// 2048, bfloat16; 256 x 256 tiles of 8 waves, one workgroup a CU); bank conflicts are at most
+// 1% of the LDS cycles (3.7% in dx_kernel, at the tile's end).  A tile's first loads and its end,
+// 4 to 10 us, overlap with no products.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -47,7 +48,6 @@ struct Half<_Float16> {
 };
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ f32x4 product(Half<__bf16>::v8 a, Half<__bf16>::v8 b, f32x4 c)
 {
@@ -292,9 +292,10 @@ struct TileProduct {
         half_step(1, a_s2, b_s2, places_a, places_b, f, acc);   // (at the end: of what is not used)
     }
 
-    // Different buffers are told apart by `restrict`: otherwise the compiler has every read wait for all
-    // loads to LDS.  Where both k are adjacent, each buffer is in its place again after four steps (s
-    // a multiple of 4); else the four of m or n adjacent are all different within two.
+    // Different buffers are told apart by `restrict`: otherwise the compiler has every read wait
+    // for all loads to LDS.  Where both k are adjacent, each buffer is in its place again after
+    // four steps (s a multiple of 4); else the four of m or n adjacent are all different within
+    // two.
     static __device__ __forceinline__ void four_steps(A &sa, B &sb, int s, int steps, int wave,
                                                       char *__restrict__ a0, char *__restrict__ a1,
                                                       char *__restrict__ b0, char *__restrict__ b1,

@@ -18,8 +18,8 @@
 //    join_kernel joins the cuts.  Bound by memory in large calls (bfloat16: 8192 x 65536 in 177 us,
 //    6.1 TB/s; 262144 x 1024 in 87 us, 6.2 TB/s) with the vector units close behind: 16-bit
 //    logits take about a conversion, a maximum, two fused multiply-adds, an addition and an
-//    exponential each.  A single row of 65536 with its 20 best takes 13 us, of which the
-//    selection's dependent steps are most.
+//    exponential each.  A single row of 65536 takes 6 us without alternatives and 12 with its
+//    20 best: the selection's dependent steps are half.
 //  * The k best entries: every lane keeps the largest entry of each of its groups of vectors,
 //    with the vector it first appeared in.  The lanes' best are sorted; the k-th of them bounds
 //    the k-th entry of the row, and the few groups that reach it are read again (from the cache)
@@ -27,7 +27,8 @@
 //    first) make every order strict, so ties need nothing of their own, and the cost hardly
 //    depends on the data.  Sorting goes through registers (DPP and row swaps), not LDS.
 //    4096 x 32768 bfloat16: 40 us without, 77 us with the 64 best.  Many short rows are bound by
-//    the sorts' instructions (262144 x 500: 79 us, 535 with the 5 best).
+//    instructions (262144 x 500: 87 us, 521 with the 5 best): two sorts of 64 keys for each row (three
+//    and a merge above 16 best), and blocks of 4 vectors a lane where a row has one.
 //  * grad_kernel: one pass, element by element; the given token's term is added by the lane that
 //    owns it, and the teacher's tokens are written once more by the wave that wrote their
 //    neighbours, so no atomics are needed.  Bound by memory: 8192 x 65536 bfloat16 takes 489 us
@@ -54,7 +55,10 @@ constexpr int64_t kMaxGrid = 1 << 20;   // workgroups of a launch; they loop ove
 constexpr int64_t kFillWaves = 2048;    // waves wanted: rows get several where they are few
 constexpr int64_t kLongVecs = 4096;     // vectors of a row that 4 waves share in any case
 constexpr int64_t kWaveVecs = 128;      // vectors for each of a row's waves, at least
-// Vectors (512 KB) that one workgroup reads about as fast as another launch would join cuts.
+// Vectors (512 KB) up to which a row is one workgroup's.  Cuts of 32 KB and their join take less on
+// the GPU (32 rows of 100000 float32 with 8 best: 12 + 4 us instead of 19; one row of 65536 with 20
+// best 10 + 4 instead of 12), but a second launch and a workspace on the host, which bounds
+// such calls: 23.5 us instead of 19.5, and 23.6 instead of 19.2.
 constexpr int64_t kCutVecs = 32768;
 constexpr int kMaxCuts = 64;
 // Gradients that do not fit in the last cache together with their logits go past the
