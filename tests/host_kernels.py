@@ -103,5 +103,8 @@ def in_child(target, *args):
     """In a process of its own: an access outside a buffer ends it with a signal."""
     p = multiprocessing.get_context("fork").Process(target=target, args=args)
     p.start()
-    p.join()
+    p.join(300)
+    if p.exitcode is None:
+        p.kill()
+        p.join()
     assert p.exitcode == 0, f"exit code {p.exitcode}"
